@@ -119,10 +119,12 @@ fp_status vocab_loss_forward(const void* x, int64_t x_stride, const void* weight
  *   g[t][v] = (exp(z[t][v] - lse[t]) - (v == label[t])) * dloss (/ n for
  *   FP_LOSS_MEAN) for labelled rows:
  *   dx = g weight (rows without a label: zero),  dweight = transposed g x.
- * The logits are formed again, piece by piece. exp(z - lse) is rounded to
- * `type` for the two products, as x and weight are; their sums are f32, and
- * the factor dloss / n is applied to them. What rounding takes from a row's
- * g at its label is put back into dx.
+ * The logits are formed again, piece by piece. exp(z - lse) of the classes
+ * that are not the row's label is rounded to `type` for the two products, as x
+ * and weight are; their sums are f32, and the factor dloss / n is applied to
+ * them. g at the label is minus the f32 sum of the row's other exp(z - lse),
+ * so that it keeps its relative accuracy where the label is nearly certain; its
+ * parts of dx and dweight are added in f32.
  *  lse           what vocab_loss_forward wrote for the same x, weight, labels.
  *  dloss         device f32 [1], the gradient of the loss; NULL = 1.
  *  dx            device, `type` [rows, hidden], row stride dx_stride, or NULL.

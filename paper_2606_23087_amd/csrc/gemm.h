@@ -520,7 +520,8 @@ __device__ __forceinline__ void rows_out(const Packed& x, int j, char* own, Sink
   wave_order();
 }
 
-// The sums themselves times `scale`, all 128 rows: 4 values of 32 bits at a time.
+// The sums themselves times `scale`, all 128 rows, 32 rows of Q (the j-th) after
+// the other: sink(j, q, p, vector) with 4 values of 32 bits at a time.
 template <class Sink>
 __device__ __forceinline__ void rows_out(const Acc& acc, float scale, char* own, Sink sink) {
   const int lane = threadIdx.x & 63;
@@ -541,7 +542,7 @@ __device__ __forceinline__ void rows_out(const Acc& acc, float scale, char* own,
 #pragma unroll
       for (int k = 0; k < 8; ++k) {
         const int q = k * 4 + (lane >> 4), v = lane & 15;
-        sink(wave_q() + j * 32 + q, wave_p() + half * 64 + v * 4, *(const f32x4*)(own + q * 256 + ((v ^ (q & 15)) << 4)));
+        sink(j, wave_q() + j * 32 + q, wave_p() + half * 64 + v * 4, *(const f32x4*)(own + q * 256 + ((v ^ (q & 15)) << 4)));
         if (k & 1) __builtin_amdgcn_sched_barrier(0);
       }
       wave_order();

@@ -17,12 +17,15 @@
 // so the reduction is nearly all within a lane.
 //
 // Backward: pieces of the vocabulary, each three products: the logits again,
-// with the epilogue making exp(z - lse), less 1 at the label, rounded to 16
-// bits; then its products with the piece's weight (added up in f32 over pieces)
-// and with the rows (the piece's rows of dweight, final). A piece has as many
-// classes as the labelled rows leave room for, so the fewer rows there are, the
-// fewer pieces; the host enqueues as many as all rows would make, and those
-// past the vocabulary end at once.
+// with the epilogue making exp(z - lse), rounded to 16 bits, and 0 at the label;
+// then its products with the piece's weight (added up in f32 over pieces) and
+// with the rows (the piece's rows of dweight). A piece has as many classes as
+// the labelled rows leave room for, so the fewer rows there are, the fewer
+// pieces; the host enqueues as many as all rows would make, and those past the
+// vocabulary end at once. The gradient at a row's label is known once all pieces
+// are done: then k_finish adds its parts of dx and of the classes that are
+// labels, whose sums waited in f32 (a counting sort of the labelled rows says
+// which rows a class has).
 //
 // Measured (bf16): the loss of 4096 labelled rows over 152064 x 4096 3.93 ms, 1300
 // TFLOP/s; a step of 4096 over 152064 x 3584 14.4 ms, of 8192 over 128256 x 5120
@@ -109,13 +112,101 @@ __global__ __launch_bounds__(1024) void k_label_rows(const int32_t* labels, int3
   }
 }
 
+// The labelled rows by class, for the sums of each class's own rows.
+struct Classes {
+  int32_t* order;               // [labelled rows]: the rows, by class and then by number
+  int32_t* many;                // of the class that begins at this place of order: its rows; 0 at the places behind
+  int32_t* begin;               // [vocab]: a class's place in order, -1 for one that is no row's label
+};
+
+// Orders the rows of the `tile`-th 256 classes: a stable counting sort, whose
+// place among all classes is the number of rows below the tile. Each of 4 waves
+// has a quarter of the rows, in their order.
+__device__ __forceinline__ void order_classes(const Classes& o, int32_t tile, const int32_t* picks, int32_t n, int32_t vocab) {
+  __shared__ int32_t at[4][256], first[256], total[256], sums[8];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) at[w][threadIdx.x] = 0;
+  __syncthreads();
+  const int32_t quarter = (n + 255) / 256 * 64, from = min(wave * quarter, n), to = min(from + quarter, n), v0 = tile * 256;
+  int32_t below = 0;
+  for (int32_t i = from + lane; i < to; i += 256) {
+    int32_t c[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) c[e] = i + 64 * e < to ? picks[i + 64 * e] - v0 : 256;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      below += c[e] < 0;
+      if ((uint32_t)c[e] < 256u) atomicAdd(&at[wave][c[e]], 1);
+    }
+  }
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) below += __shfl_xor(below, d);
+  if (lane == 0) sums[wave] = below;
+  __syncthreads();
+  int32_t mine = 0;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) mine += at[w][threadIdx.x];
+  int32_t before = mine;                         // inclusive over the wave
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) {
+    const int32_t o2 = __shfl_up(before, d);
+    if (lane >= d) before += o2;
+  }
+  if (lane == 63) sums[4 + wave] = before;
+  __syncthreads();
+  int32_t place = before - mine + sums[0] + sums[1] + sums[2] + sums[3];
+#pragma unroll
+  for (int w = 0; w < 4; ++w)
+    if (w < wave) place += sums[4 + w];
+  first[threadIdx.x] = place;
+  total[threadIdx.x] = mine;
+  if (v0 + (int)threadIdx.x < vocab) o.begin[v0 + threadIdx.x] = mine ? place : -1;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    const int32_t here = at[w][threadIdx.x];
+    at[w][threadIdx.x] = place;
+    place += here;
+  }
+  __syncthreads();
+  for (int32_t base = from; base < to; base += 256) {
+    int32_t c[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) c[e] = base + 64 * e + lane < to ? picks[base + 64 * e + lane] - v0 : 256;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const bool in = (uint32_t)c[e] < 256u;
+      uint64_t same = __ballot(in);              // lanes with this lane's class
+      if (!same) continue;
+#pragma unroll
+      for (int b = 0; b < 8; ++b) {
+        const bool bit = c[e] >> b & 1;
+        const uint64_t set = __ballot(bit);
+        same &= bit ? set : ~set;
+      }
+      const int32_t rank = __popcll(same & ((1ull << lane) - 1));
+      if (in) {
+        const int32_t to_place = at[wave][c[e]] + rank;
+        o.order[to_place] = base + 64 * e + lane;
+        o.many[to_place] = to_place == first[c[e]] ? total[c[e]] : 0;
+      }
+      wave_order();
+      if (in && rank == 0) at[wave][c[e]] += __popcll(same);
+      wave_order();
+    }
+  }
+}
+
 // Gathers the labelled rows into xc [.., ld], zeros from hidden to ld, and with
 // them (backward) their lse. Past the last row nothing is written: those rows
-// of a tile are read as the last one, and left out of every result.
+// of a tile are read as the last one, and left out of every result. Workgroups
+// past the n_rows-th order the rows by class, a tile of classes each.
 template <class T>
 __global__ __launch_bounds__(256) void k_gather_rows(const T* x, int64_t x_stride, const int32_t* rows, const int32_t* count,
-                                                     int32_t hidden, int32_t ld, T* xc, const float* lse, float* lses) {
+                                                     int32_t hidden, int32_t ld, T* xc, const float* lse, float* lses, int32_t n_rows,
+                                                     const int32_t* picks, int32_t vocab, Classes classes) {
   const int32_t i = blockIdx.x;
+  if (i >= n_rows) return order_classes(classes, i - n_rows, picks, *count, vocab);
   if (i >= *count) return;
   if (lse && threadIdx.x == 0) lses[i] = lse[rows[i]];
   const T* src = x + (int64_t)rows[i] * x_stride;
@@ -146,10 +237,14 @@ struct LossArgs {
   const float* lses;            // of the labelled rows
   void* g;                      // the piece's gradient of the logits [rows][classes of a piece]
   int64_t room;                 // elements of g
-  float* rest;                  // what rounding took from each row's gradient at its label
+  float* others;                // [128 classes][rows]: sums of the other classes' gradients
+  int32_t others_ld;
+  const float* own;             // each row's gradient at its label
   int32_t u;                    // the piece's number
   float* sum;                   // dx's sums [split][rows][ld]
   int64_t sum_rows;             // of all splits
+  const int32_t* begin;         // as in Classes
+  float* side;                  // dweight's sums of classes that are labels, at their place of order [rows][ld]
 };
 
 // Classes of a piece with n labelled rows: whole tiles, pieces as even as that
@@ -443,30 +538,43 @@ __device__ __forceinline__ void narrow_backward(const LossArgs& a, const Piece& 
   const auto finish = [&](int32_t id, NarrowAcc<kJ>& acc) {
     const int32_t tq = id / pt * (32 * kJ), tp = id % pt, v0 = tp * kTile + wave * 64 + lane_p();
     T* const to = (T*)a.g + (int64_t)tq * c.ld + tp * kTile + wave * 64;
+    // each wave's sums of a row, behind what narrow_rows_out uses
+    const auto sums = [&](int w) { return (float*)(lds + kOwnAt + w * kOwnBytes + kOwnBytes / 2); };
 #pragma unroll
     for (int j = 0; j < kJ; ++j) {
       uint32_t w[2][8];
-      float z[32];
+      float z[32], y[2] = {0.f, 0.f};
 #pragma unroll
       for (int i = 0; i < 32; ++i) {
-        const int32_t v = v0 + i / 4 * 8 + i % 4, t = tq + lane_q() + j * 32;
+        const int32_t v = v0 + i / 4 * 8 + i % 4;
         z[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(sum_of(acc, i >> 4, j, i & 15), kLog2e, lift[j]));
-        if (v == pick[j] && t < n) {
-          z[i] -= (float)(1 << kLift<T>);
-          a.rest[t] = z[i] - (float)(T)z[i];
-        }
-        if (t >= n || v >= c.classes) z[i] = 0.f;
+        if (tq + lane_q() + j * 32 >= n || v >= c.classes || v == pick[j]) z[i] = 0.f;
+        y[i & 1] += z[i];
       }
+      const float s = y[0] + y[1], both = s + __shfl_xor(s, 32);
+      sums(wave)[j * 32 + lane_q()] = both;      // the same from both lanes
 #pragma unroll
       for (int i = 0; i < 16; ++i) w[i >> 3][i & 7] = pack2<T>(z[2 * i], z[2 * i + 1]);
       narrow_rows_out(w, j, lds + kOwnAt + wave * kOwnBytes, [&](int q, int p, u32x4 v) { *(u32x4*)(to + (int64_t)q * c.ld + p) = v; });
+    }
+    barrier();
+    if ((int)threadIdx.x < min(n - tq, 32 * kJ)) {
+      float* const others = a.others + (int64_t)(c.first / kTile + tp) * 2 * a.others_ld + tq + threadIdx.x;
+      others[0] = sums(0)[threadIdx.x] + sums(1)[threadIdx.x];
+      others[a.others_ld] = sums(2)[threadIdx.x] + sums(3)[threadIdx.x];
     }
   };
   walk(pt * qt, lds_address(lds), g, begin, take, finish);
 }
 
-// The piece's gradient of the logits (without dloss / n): exp(z - lse), minus
-// 1 at the label; zeros past the labelled rows and classes.
+// The piece's gradient of the logits (without dloss / n): exp(z - lse); zeros at
+// the label, past the labelled rows and past the classes. The gradient at the
+// label, exp(z - lse) - 1, is minus the sum of the row's others, whose parts of
+// 128 classes are kept in f32: it is complete with the last piece alone, but has
+// the relative accuracy of its terms, where the subtraction would leave nothing
+// of it for a label that is nearly certain (an error of 1e-6 at logits of 28,
+// where the gradient may be 1e-7). Being as large as all others of its row
+// together, it takes no part in the 16-bit products: their results get it in f32.
 template <class T>
 __global__ __launch_bounds__(kGemmThreads, 1) void k_logits_backward(LossArgs a) {
   __shared__ __align__(1024) char lds[kGemmLds];
@@ -511,20 +619,21 @@ __global__ __launch_bounds__(kGemmThreads, 1) void k_logits_backward(LossArgs a)
 #pragma unroll
       for (int i = 0; i < 64; ++i) z[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(sum_of(acc, i >> 4, j, i & 15), kLog2e, lift[j]));
       if (at[j] >= 0 && at[j] < 128 && (at[j] & 7) < 4) {
-        float own_g = 0.f;
 #pragma unroll
-        for (int i = 0; i < 64; ++i) {
-          const bool is = at[j] == i / 4 * 8 + i % 4;
-          z[i] -= is ? (float)(1 << kLift<T>) : 0.f;
-          own_g = is ? z[i] : own_g;
-        }
-        a.rest[t0 + j * 32] = own_g - (float)(T)own_g;
+        for (int i = 0; i < 64; ++i)
+          if (at[j] == i / 4 * 8 + i % 4) z[i] = 0.f;
       }
       if (tp + kTile > c.classes || tq + kTile > n) {
 #pragma unroll
         for (int i = 0; i < 64; ++i)
           if (t0 + j * 32 >= n || v0 + i / 4 * 8 + i % 4 >= c.classes) z[i] = 0.f;
       }
+      float y[2] = {0.f, 0.f};
+#pragma unroll
+      for (int i = 0; i < 64; ++i) y[i & 1] += z[i];
+      const float s = y[0] + y[1], both = s + __shfl_xor(s, 32);
+      if ((threadIdx.x & 63) < 32 && t0 + j * 32 < n)
+        a.others[(int64_t)((c.first + tp + wave_p()) / 128) * a.others_ld + t0 + j * 32] = both;
       Packed x;
 #pragma unroll
       for (int i = 0; i < 32; ++i) x.w[i >> 3][i & 7] = pack2<T>(z[2 * i], z[2 * i + 1]);
@@ -533,6 +642,22 @@ __global__ __launch_bounds__(kGemmThreads, 1) void k_logits_backward(LossArgs a)
     }
   };
   walk(pt * qt, lds_address(lds), g, begin, take, finish);
+}
+
+// Each labelled row's gradient at its label, from the others' sums: 64 threads a
+// row, as in k_lse.
+__global__ __launch_bounds__(1024) void k_own_gradient(const float* others, int32_t ld, int32_t parts, const int32_t* count, float* own) {
+  const int32_t n = *count, t0 = blockIdx.x * 16;
+  __shared__ float lds[64][17];
+  if (t0 >= n) return;
+  float s = 0.f;
+  if (t0 + (int)(threadIdx.x & 15) < n)
+    for (int32_t i = threadIdx.x >> 4; i < parts; i += 64) s += others[(int64_t)i * ld + t0 + (threadIdx.x & 15)];
+  lds[threadIdx.x >> 4][threadIdx.x & 15] = s;
+  __syncthreads();
+  s = reduce64<Add>(lds[threadIdx.x & 63][threadIdx.x >> 6]);
+  const int32_t t = t0 + (threadIdx.x >> 6);
+  if ((threadIdx.x & 63) == 0 && t < n) own[t] = -s;
 }
 
 // How many workgroups share a tile of dx, each with a part of the piece's
@@ -609,7 +734,7 @@ __global__ __launch_bounds__(kGemmThreads, 1) void k_rows_gradient(LossArgs a) {
     char* const own = lds + kOwnAt + (threadIdx.x >> 6) * kOwnBytes;
     const int64_t ld = here(a.ld);
     float* const to = a.sum + ((int64_t)split * qt * kTile + tq) * ld + tp;
-    rows_out(acc, 1.f, own, [&](int q, int p, f32x4 v) {
+    rows_out(acc, 1.f, own, [&](int, int q, int p, f32x4 v) {
       if (tq + q >= n || tp + p >= a.hidden) return;
       f32x4* const at = (f32x4*)(to + (int64_t)q * ld + p);
       *at = a.u ? *at + v : v;
@@ -625,7 +750,8 @@ __device__ __forceinline__ float factor(const float* dloss, const int32_t* count
   return mean ? d / (float)max(*count, 1) : d;
 }
 
-// The piece's rows of dweight: (+)= factor * transposed g x.
+// The piece's rows of dweight: (+)= factor * transposed g x. Classes that are some
+// row's label leave their sums in f32 for k_finish.
 template <class T, class O>
 __global__ __launch_bounds__(kGemmThreads, 1) void k_weight_gradient(LossArgs a, const float* dloss, int32_t mean, O* dweight,
                                                                      int64_t dw_ld, int32_t add) {
@@ -636,10 +762,17 @@ __global__ __launch_bounds__(kGemmThreads, 1) void k_weight_gradient(LossArgs a,
   const float f = factor<T>(dloss, a.count, mean);
   const Operand16 P{a.xc, a.ld, a.hidden, n}, Q{a.g, c.ld, qt * kTile, n};
   Gemm<T, true, true> g;
+  int32_t next[4] = {}, side[4];   // where the lane's classes leave their sums: of the tile whose loads are under way, of the one that is ready
   const auto begin = [&](int32_t id) {
     int32_t p, q;
     tile_of(id, pt, qt, &p, &q);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) next[j] = a.begin[c.first + min(q + wave_q() + lane_q() + j * 32, c.classes - 1)];
     g.start(P, Q, a.zeros, p, q, lds_address(lds));
+  };
+  const auto take = [&] {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) side[j] = next[j];
   };
   const auto finish = [&](int32_t id, Acc& acc) {
     int32_t tp, tq;
@@ -647,9 +780,24 @@ __global__ __launch_bounds__(kGemmThreads, 1) void k_weight_gradient(LossArgs a,
     char* const own = lds + kOwnAt + (threadIdx.x >> 6) * kOwnBytes;
     const int64_t ld = here(dw_ld);
     O* const to = dweight + (c.first + (int64_t)tq) * ld + tp;
+    uint32_t labels[4];            // which of the wave's 32 classes are
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      if (tq + wave_q() + lane_q() + j * 32 >= c.classes) side[j] = -1;
+      labels[j] = (uint32_t)__ballot(side[j] >= 0);
+      if (!labels[j]) continue;
+      float* const row = a.side + (int64_t)side[j] * a.ld + tp + wave_p() + lane_p();
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        f32x4 v;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = sum_of(acc, i >> 2, j, 4 * (i & 3) + e);
+        if (side[j] >= 0 && tp + wave_p() + lane_p() + i * 8 < a.hidden) *(f32x4*)(row + i * 8) = v;
+      }
+    }
     if constexpr (__is_same(O, float)) {
-      rows_out(acc, f, own, [&](int q, int p, f32x4 v) {
-        if (tq + q >= c.classes || tp + p >= a.hidden) return;
+      rows_out(acc, f, own, [&](int j, int q, int p, f32x4 v) {
+        if (tq + q >= c.classes || tp + p >= a.hidden || (labels[j] >> (q & 31) & 1)) return;
         f32x4* const at = (f32x4*)(to + (int64_t)q * ld + p);
         *at = add ? *at + v : v;
       });
@@ -666,20 +814,15 @@ __global__ __launch_bounds__(kGemmThreads, 1) void k_weight_gradient(LossArgs a,
       }
     }
   };
-  walk(pt * qt, lds_address(lds), g, begin, [] {}, finish);
+  walk(pt * qt, lds_address(lds), g, begin, take, finish);
 }
 
-// dx: the splits' sums times the factor; zeros for rows without a label. The
-// gradient at the label is as large as all others of its row together, so its
-// rounding to 16 bits would scale the whole row (up to 2^-9 in bf16): the rest
-// is put back here. The others' roundings average out.
+// A row of dx: the label's gradient times its weight and the splits' sums, times
+// the factor; zeros for rows without a label. 2048 columns a workgroup.
 template <class T>
-__global__ __launch_bounds__(256) void k_rows_finish(LossArgs a, const int32_t* slot, const float* dloss, int32_t mean, T* dx,
-                                                     int64_t dx_stride) {
-  const int32_t t = blockIdx.x, i = slot[t], n = *a.count;
+__device__ __forceinline__ void finish_row(const LossArgs& a, int32_t t, int32_t i, float f, T* dx, int64_t dx_stride) {
   T* out = dx + (int64_t)t * dx_stride;
-  const float f = factor<T>(dloss, a.count, mean);
-  const int32_t tile = rows_of_sum(n), rows = (n + tile - 1) / tile * tile;
+  const int32_t n = *a.count, tile = rows_of_sum(n), rows = (n + tile - 1) / tile * tile;
   const int32_t splits = i < 0 ? 0 : splits_of((a.hidden + kTile - 1) / kTile, rows / tile, tile, piece_of(n, a.vocab, a.room), a.sum_rows);
   const int32_t c = (blockIdx.y * 256 + threadIdx.x) * 8;
   if (c < a.hidden) {
@@ -687,9 +830,9 @@ __global__ __launch_bounds__(256) void k_rows_finish(LossArgs a, const int32_t* 
     float s[8] = {0, 0, 0, 0, 0, 0, 0, 0};
     if (i >= 0) {
       const Pack<T, 8> w = load<T, 8>((const T*)a.weight + a.picks[i] * a.weight_ld + c);
-      const float rest = a.rest[i];
+      const float own = a.own[i];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) s[e] = rest * w.get(e);
+      for (int e = 0; e < 8; ++e) s[e] = own * w.get(e);
     }
 #pragma unroll 8
     for (int32_t k = 0; k < splits; ++k) {
@@ -703,6 +846,70 @@ __global__ __launch_bounds__(256) void k_rows_finish(LossArgs a, const int32_t* 
   }
 }
 
+// The row of dweight of the class whose rows begin at place i: its sums over the
+// piece's product, and each of its own rows times that row's gradient at the
+// label. 512 columns at a time; each of 4 waves adds up every fourth row, 8 under
+// way, and the first one joins them.
+template <class T, class O>
+__device__ __forceinline__ void finish_class(const LossArgs& a, const Classes& o, int32_t i, float f, O* dweight, int64_t dw_ld,
+                                             int32_t add) {
+  __shared__ float parts[3][8][64];
+  const int32_t many = uniform(o.many[i]);
+  if (!many) return;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int64_t v = a.picks[o.order[i]];
+  for (int32_t c0 = blockIdx.y * 2048; c0 < min(a.hidden, (int32_t)(blockIdx.y + 1) * 2048); c0 += 512) {
+    const int32_t c = c0 + lane * 8, at = min(c, a.hidden - 8);
+    float s[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+    for (int32_t k = wave; k < many; k += 32) {
+      int32_t row[8];
+      float own[8];
+      Pack<T, 8> x[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) row[e] = o.order[i + min(k + 4 * e, many - 1)];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        own[e] = k + 4 * e < many ? a.own[row[e]] : 0.f;
+        x[e] = load<T, 8>((const T*)a.xc + (int64_t)row[e] * a.ld + at);
+      }
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (k + 4 * e < many)
+#pragma unroll
+          for (int d = 0; d < 8; ++d) s[d] += own[e] * x[e].get(d);
+    }
+    if (wave)
+#pragma unroll
+      for (int d = 0; d < 8; ++d) parts[wave - 1][d][lane] = s[d];
+    __syncthreads();
+    if (!wave && c < a.hidden) {
+      const Pack<float, 8> p = load<float, 8>(a.side + (int64_t)i * a.ld + c);
+      O* const to = dweight + v * dw_ld + c;
+      Pack<O, 8> out;
+      Pack<float, 8> old{};
+      if constexpr (__is_same(O, float))
+        if (add) old = load<float, 8>(to);
+#pragma unroll
+      for (int d = 0; d < 8; ++d)
+        out.set(d, old.get(d) + f * (p.get(d) + (((s[d] + parts[0][d][lane]) + parts[1][d][lane]) + parts[2][d][lane])));
+      store<O, 8>(to, out);
+    }
+    __syncthreads();
+  }
+}
+
+// What the pieces left: workgroups up to dx_rows have a row of dx each, those
+// behind a place in the order of the labelled rows.
+template <class T, class O>
+__global__ __launch_bounds__(256) void k_finish(LossArgs a, Classes o, const int32_t* slot, const float* dloss, int32_t mean, int32_t dx_rows,
+                                                T* dx, int64_t dx_stride, O* dweight, int64_t dw_ld, int32_t add) {
+  const float f = factor<T>(dloss, a.count, mean);
+  if ((int32_t)blockIdx.x < dx_rows)
+    finish_row(a, blockIdx.x, slot[blockIdx.x], f, dx, dx_stride);
+  else if ((int32_t)blockIdx.x - dx_rows < *a.count)
+    finish_class<T>(a, o, blockIdx.x - dx_rows, f, dweight, dw_ld, add);
+}
+
 // ------------------------------------------------------------------ host
 
 // Where the parts of the workspace lie (byte offsets).
@@ -710,7 +917,7 @@ struct Plan {
   int64_t rows_p;               // rows up to whole tiles
   int32_t ld;                   // hidden up to whole pairs of stages
   int64_t room, sum_rows;       // as in LossArgs
-  int64_t zeros, count, rows, picks, slot, lses, picked, row_loss, part, xc, g, sum, rest;
+  int64_t zeros, count, rows, picks, slot, lses, picked, row_loss, part, xc, g, sum, own, others, side, order, many, begin;
   int64_t bytes;
 };
 
@@ -744,7 +951,12 @@ Plan plan_of(int64_t rows, int32_t hidden, int32_t vocab, bool backward) {
     p.g = take(p.room * 2);
     p.sum_rows = std::max<int64_t>(2 * p.rows_p, kMaxSplits * kTile);
     p.sum = take(p.sum_rows * p.ld * 4);
-    p.rest = take(4 * p.rows_p);
+    p.own = take(4 * p.rows_p);
+    p.others = take(2 * tiles * p.rows_p * 4);
+    p.side = take(p.rows_p * p.ld * 4);
+    p.order = take(4 * p.rows_p);
+    p.many = take(4 * p.rows_p);
+    p.begin = take(4 * (int64_t)vocab);
     p.bytes = std::max(p.bytes, at);
   }
   return p;
@@ -778,17 +990,19 @@ fp_status check(const char* what, const void* x, int64_t x_stride, const void* w
   return FP_OK;
 }
 
-// What both passes begin with: zeros, the list of labelled rows, their gather.
+// What both passes begin with: zeros, the list of labelled rows, their gather, and (with `classes`) their order.
 template <class T>
 hipError_t begin(const Plan& p, char* ws, const void* x, int64_t x_stride, const int32_t* labels, int64_t rows, int32_t hidden,
-                 int32_t vocab, int32_t* slot, int32_t* count_out, float* zero_lse, const float* lse, hipStream_t s) {
+                 int32_t vocab, int32_t* slot, int32_t* count_out, float* zero_lse, const float* lse, const Classes& classes, hipStream_t s) {
   int32_t* const count = (int32_t*)(ws + p.count);
   int32_t* const list = (int32_t*)(ws + p.rows);
   hipError_t e = launch(k_label_rows, dim3(1), dim3(1024), 0, s, labels, (int32_t)rows, vocab, list, (int32_t*)(ws + p.picks), slot,
                         count, count_out, zero_lse, (u32x4*)(ws + p.zeros));
-  if (e == hipSuccess && rows)
-    e = launch(k_gather_rows<T>, dim3((unsigned)rows), dim3(256), 0, s, (const T*)x, x_stride, (const int32_t*)list,
-               (const int32_t*)count, hidden, p.ld, (T*)(ws + p.xc), lse, (float*)(ws + p.lses));
+  const int64_t groups = rows + (classes.order ? (vocab + 255) / 256 : 0);
+  if (e == hipSuccess && groups)
+    e = launch(k_gather_rows<T>, dim3((unsigned)groups), dim3(256), 0, s, (const T*)x, x_stride, (const int32_t*)list,
+               (const int32_t*)count, hidden, p.ld, (T*)(ws + p.xc), lse, (float*)(ws + p.lses), (int32_t)rows,
+               (const int32_t*)(ws + p.picks), vocab, classes);
   return e;
 }
 
@@ -810,7 +1024,7 @@ template <class T>
 hipError_t forward(const Plan& p, char* ws, const void* x, int64_t x_stride, const void* weight, int64_t weight_stride,
                    const int32_t* labels, int64_t rows, int32_t hidden, int32_t vocab, int32_t reduction, float* loss, float* lse,
                    int32_t* n_labelled, hipStream_t s) {
-  hipError_t e = begin<T>(p, ws, x, x_stride, labels, rows, hidden, vocab, nullptr, n_labelled, lse, nullptr, s);
+  hipError_t e = begin<T>(p, ws, x, x_stride, labels, rows, hidden, vocab, nullptr, n_labelled, lse, nullptr, Classes{}, s);
   LossArgs a = loss_args(p, ws, weight, weight_stride, hidden, vocab);
   a.part = (float2*)(ws + p.part), a.part_ld = (int32_t)p.rows_p, a.picked = (float*)(ws + p.picked);
   float* const row_loss = (float*)(ws + p.row_loss);
@@ -832,10 +1046,14 @@ hipError_t backward(const Plan& p, char* ws, const void* x, int64_t x_stride, co
                     int32_t reduction, void* dx, int64_t dx_stride, void* dweight, int64_t dw_stride, bool dw_f32, bool add,
                     hipStream_t s) {
   int32_t* const slot = (int32_t*)(ws + p.slot);
-  hipError_t e = begin<T>(p, ws, x, x_stride, labels, rows, hidden, vocab, slot, nullptr, nullptr, lse, s);
+  Classes classes{};
+  if (dweight) classes = {(int32_t*)(ws + p.order), (int32_t*)(ws + p.many), (int32_t*)(ws + p.begin)};
+  hipError_t e = begin<T>(p, ws, x, x_stride, labels, rows, hidden, vocab, slot, nullptr, nullptr, lse, classes, s);
   LossArgs a = loss_args(p, ws, weight, weight_stride, hidden, vocab);
   const int32_t mean = reduction == FP_LOSS_MEAN;
-  a.lses = (float*)(ws + p.lses), a.g = ws + p.g, a.room = p.room, a.sum = (float*)(ws + p.sum), a.sum_rows = p.sum_rows, a.rest = (float*)(ws + p.rest);
+  a.lses = (float*)(ws + p.lses), a.g = ws + p.g, a.room = p.room, a.sum = (float*)(ws + p.sum), a.sum_rows = p.sum_rows;
+  a.others = (float*)(ws + p.others), a.others_ld = (int32_t)p.rows_p, a.own = (float*)(ws + p.own);
+  a.begin = classes.begin, a.side = (float*)(ws + p.side);
   // with all rows labelled there are the most pieces
   const int32_t most = piece_of(rows, vocab, p.room);
   const int64_t pieces = ((int64_t)vocab + most - 1) / most;
@@ -851,8 +1069,17 @@ hipError_t backward(const Plan& p, char* ws, const void* x, int64_t x_stride, co
         e = launch(k_weight_gradient<T, T>, grid, dim3(kGemmThreads), 0, s, a, dloss, mean, (T*)dweight, dw_stride, 0);
     }
   }
-  if (rows && dx && e == hipSuccess)
-    e = launch(k_rows_finish<T>, dim3((unsigned)rows, (unsigned)((hidden + 2047) / 2048)), dim3(256), 0, s, a, (const int32_t*)slot, dloss, mean, (T*)dx, dx_stride);
+  if (!rows) return e;
+  if (e == hipSuccess)
+    e = launch(k_own_gradient, dim3((unsigned)((rows + 15) / 16)), dim3(1024), 0, s, (const float*)a.others, a.others_ld,
+               (int32_t)(2 * tiles(vocab)), a.count, (float*)(ws + p.own));
+  const auto finish = [&](auto* dw) {
+    using O = std::remove_pointer_t<decltype(dw)>;
+    const dim3 grid((unsigned)((dx ? rows : 0) + (dweight ? rows : 0)), (unsigned)((hidden + 2047) / 2048));
+    return launch(k_finish<T, O>, grid, dim3(256), 0, s, a, classes, (const int32_t*)slot, dloss, mean, (int32_t)(dx ? rows : 0), (T*)dx,
+                  dx_stride, dw, dw_stride, (int32_t)add);
+  };
+  if (e == hipSuccess) e = dw_f32 ? finish((float*)dweight) : finish((T*)dweight);
   return e;
 }
 
