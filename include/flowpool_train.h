@@ -126,7 +126,8 @@ fp_status vocab_loss_forward(const void* x, int64_t x_stride, const void* weight
  * so that it keeps its relative accuracy where the label is nearly certain; its
  * parts of dx and dweight are added in f32.
  *  lse           what vocab_loss_forward wrote for the same x, weight, labels.
- *  dloss         device f32 [1], the gradient of the loss; NULL = 1.
+ *  dloss         device f32 [1], the gradient of the loss; NULL = 1. If it is
+ *                not finite it reaches the labelled rows' results alone.
  *  dx            device, `type` [rows, hidden], row stride dx_stride, or NULL.
  *  dweight       device, dweight_type (`type`, or FP_F32) [vocab, hidden], row
  *                stride dweight_stride, or NULL (a frozen weight).

@@ -743,11 +743,13 @@ __global__ __launch_bounds__(kGemmThreads, 1) void k_rows_gradient(LossArgs a) {
   walk(c.classes > 0 ? pt * qt * splits : 0, lds_address(lds), gemm, begin, [] {}, finish);
 }
 
-// What the sums over a gradient of the logits are multiplied with.
+// What the sums over a gradient of the logits are multiplied with. Without
+// labelled rows they are empty, whatever dloss is.
 template <class T>
 __device__ __forceinline__ float factor(const float* dloss, const int32_t* count, int32_t mean) {
+  if (*count == 0) return 0.f;
   const float d = (dloss ? *dloss : 1.f) * (1.f / (float)(1 << kLift<T>));
-  return mean ? d / (float)max(*count, 1) : d;
+  return mean ? d / (float)*count : d;
 }
 
 // The piece's rows of dweight: (+)= factor * transposed g x. Classes that are some
@@ -841,7 +843,7 @@ __device__ __forceinline__ void finish_row(const LossArgs& a, int32_t t, int32_t
       for (int e = 0; e < 8; ++e) s[e] += p.get(e);
     }
 #pragma unroll
-    for (int e = 0; e < 8; ++e) o.set(e, s[e] * f);
+    for (int e = 0; e < 8; ++e) o.set(e, i >= 0 ? s[e] * f : 0.f);      // f may be no number
     store<T, 8>(out + c, o);
   }
 }
