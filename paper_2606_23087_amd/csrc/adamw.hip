@@ -45,7 +45,11 @@ constexpr int kSteps = 4;
 constexpr int kChunk = kSteps * kStep;         // elements of a workgroup
 static_assert(FP_ADAMW_BLOCK == 64 * kVec, "a run of shared scales is a wave's");
 constexpr int kTensors = 48;                   // of one launch
-constexpr float kTiny = 0x1p-80f;              // scales below this are taken for it when codes are made
+// Runs whose scale is below kSmall are worked on times kLift, which is exact: the
+// reciprocals that lead to codes would overflow, and what one unit of a level
+// stands for would lose bits below the normal numbers.
+constexpr float kSmall = 0x1p-64f, kLift = 0x1p84f;
+constexpr float kNone = 0x1p-80f;              // below any other scale's reciprocal: for runs of zeros
 constexpr float kTopM = 127.f * 127.f, kTopV = 65025.f * 65025.f;   // 127^2, 255^4
 
 struct Tensor {
@@ -142,6 +146,8 @@ __device__ __forceinline__ uint32_t level_v(float t, float r) {
   return (uint32_t)c + (t >= above(c) * above(c) ? 1u : 0u);
 }
 
+// What a unit of the level's power stands for (times kLift for a small scale).
+__device__ __forceinline__ float unit_of(float scale, float top) { return (scale < kSmall ? scale * kLift : scale) * (1.f / top); }
 __device__ __forceinline__ float value_m(uint32_t code, float unit) {   // unit = scale / 127^2
 #pragma clang fp contract(off)
   const float c = (float)(code & 127u), q = c * c * unit;
@@ -160,7 +166,7 @@ struct Step {
   Some<P> p;
   Some<G> g;
   Some<S> m, v;
-  float um, uv;                                  // 8 bits: values of a unit of the codes' powers
+  float sm, sv;                                  // 8 bits: scales
 
   __device__ __forceinline__ void read(const Tensor& t, int64_t at, int left) {
     p.template read<kWhole>((const P*)t.param + at, left);
@@ -169,8 +175,8 @@ struct Step {
     v.template read<kWhole>((const S*)t.v + at, left);
     if constexpr (kEight) {
       // past the tensor there is no scale
-      um = kWhole || left > 0 ? t.m_scale[at / FP_ADAMW_BLOCK] * (1.f / kTopM) : 0.f;
-      uv = kWhole || left > 0 ? t.v_scale[at / FP_ADAMW_BLOCK] * (1.f / kTopV) : 0.f;
+      sm = kWhole || left > 0 ? t.m_scale[at / FP_ADAMW_BLOCK] : 0.f;
+      sv = kWhole || left > 0 ? t.v_scale[at / FP_ADAMW_BLOCK] : 0.f;
     }
   }
 
@@ -178,19 +184,31 @@ struct Step {
   __device__ __forceinline__ void finish(const Rates& a, const Tensor& t, float keep, int64_t at, int left, float gs) {
 #pragma clang fp contract(off)
     float np[kVec], nm[kVec], nv[kVec], rv[kVec];
+    if constexpr (kEight) {
+      const float um = unit_of(sm, kTopM), uv = unit_of(sv, kTopV);
+#pragma unroll
+      for (int e = 0; e < kVec; ++e) {
+        nm[e] = value_m(m.a.v[e], um);
+        nv[e] = value_v(v.a.v[e], uv);
+      }
+      if (sm < kSmall)                           // all lanes of a run or none, so it costs a test as a rule
+#pragma unroll
+        for (int e = 0; e < kVec; ++e) nm[e] *= 1.f / kLift;
+      if (sv < kSmall)
+#pragma unroll
+        for (int e = 0; e < kVec; ++e) nv[e] *= 1.f / kLift;
+    } else {
+#pragma unroll
+      for (int e = 0; e < kVec; ++e) {
+        nm[e] = m.a.v[e];
+        nv[e] = v.a.v[e];
+      }
+    }
 #pragma unroll
     for (int e = 0; e < kVec; ++e) {
       const float ge = g.a.get(e) * gs;
-      float om, ov;
-      if constexpr (kEight) {
-        om = value_m(m.a.v[e], um);
-        ov = value_v(v.a.v[e], uv);
-      } else {
-        om = m.a.v[e];
-        ov = v.a.v[e];
-      }
-      nm[e] = om * a.beta1 + ge * a.om1;
-      nv[e] = ov * a.beta2 + ge * ge * a.om2;
+      nm[e] = nm[e] * a.beta1 + ge * a.om1;
+      nv[e] = nv[e] * a.beta2 + ge * ge * a.om2;
       // the update is a small part of the parameter: the hardware's root and reciprocal (1 ulp) serve it
       rv[e] = __builtin_amdgcn_sqrtf(nv[e]);
       const float away = __builtin_fmaf(rv[e], a.far, a.eps);
@@ -218,7 +236,21 @@ struct Step {
       }
       hm = reduce64<Max>(hm);
       hv = reduce64<Max>(hv);
-      const float im = 1.f / fmaxf(hm, kTiny) * kTopM, iv = 1.f / fmaxf(hv, kTiny) * kTopV;
+      float lm = hm, lv = hv;                    // what the codes are made against
+      if (hm < kSmall) {
+        lm *= kLift;
+#pragma unroll
+        for (int e = 0; e < kVec; ++e) nm[e] *= kLift;
+      }
+      if (hv < kSmall) {
+        lv *= kLift;
+#pragma unroll
+        for (int e = 0; e < kVec; ++e) {
+          nv[e] *= kLift;
+          rv[e] = __builtin_amdgcn_sqrtf(nv[e]);
+        }
+      }
+      const float im = 1.f / fmaxf(lm, kNone) * kTopM, iv = 1.f / fmaxf(lv, kNone) * kTopV;
       const float riv = __builtin_amdgcn_sqrtf(iv);
 #pragma unroll
       for (int e = 0; e < kVec; ++e) {
@@ -308,21 +340,24 @@ __global__ __launch_bounds__(64) void k_table(TableArgs a) {
 
 template <int kMoment, bool kWhole>
 __device__ __forceinline__ void values(const uint8_t* codes, const float* scales, float* out, int64_t n, int64_t start) {
+#pragma clang fp contract(off)
+  constexpr float kTop = kMoment == 1 ? kTopM : kTopV;
   Some<uint8_t> c[kSteps];
-  float unit[kSteps];
+  float scale[kSteps];
 #pragma unroll
   for (int k = 0; k < kSteps; ++k) {
     const int64_t at = start + k * kStep;
     const int left = kWhole ? kVec : (int)std::min<int64_t>(std::max<int64_t>(n - at, 0), kVec);
     c[k].read<kWhole>(codes + at, left);
-    unit[k] = left ? scales[at / FP_ADAMW_BLOCK] * (kMoment == 1 ? 1.f / kTopM : 1.f / kTopV) : 0.f;
+    scale[k] = left ? scales[at / FP_ADAMW_BLOCK] : 0.f;
   }
 #pragma unroll
   for (int k = 0; k < kSteps; ++k) {
     const int64_t at = start + k * kStep;
+    const float unit = unit_of(scale[k], kTop), lift = scale[k] < kSmall ? 1.f / kLift : 1.f;
     Some<float> f;
 #pragma unroll
-    for (int e = 0; e < kVec; ++e) f.a.v[e] = kMoment == 1 ? value_m(c[k].a.v[e], unit[k]) : value_v(c[k].a.v[e], unit[k]);
+    for (int e = 0; e < kVec; ++e) f.a.v[e] = (kMoment == 1 ? value_m(c[k].a.v[e], unit) : value_v(c[k].a.v[e], unit)) * lift;
     f.write<kWhole>(out + at, kWhole ? kVec : (int)std::min<int64_t>(std::max<int64_t>(n - at, 0), kVec));
   }
 }

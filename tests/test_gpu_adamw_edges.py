@@ -1,0 +1,90 @@
+"""AdamW's states at the ends of f32's range: runs of 8-bit states whose largest value is tiny."""
+
+import numpy as np
+import pytest
+
+from gpu_common import say
+import training_ref as ref
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+
+LEAST = 2.0 ** -149               # f32's smallest value: a result below 2^-126 is off by half of it
+
+
+@pytest.fixture(scope="module")
+def tr():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    from paper_2606_23087_amd import training
+    return training
+
+
+class State:
+    """One tensor with its state, before its first step."""
+
+    def __init__(self, tr, grad, bits, start=0.0):
+        self.tr, self.g, n = tr, grad, grad.numel()
+        self.p = torch.full((n,), start, device="cuda")
+        state = torch.uint8 if bits == 8 else torch.float32
+        self.m, self.v = (torch.zeros(n, dtype=state, device="cuda") for _ in range(2))
+        self.scales = torch.zeros(2, -(-n // 256), device="cuda") if bits == 8 else None
+        self.tensors = tr.adamw_tensors([self.p], [self.g], [self.m], [self.v], scales=None if bits == 32 else [self.scales])
+
+    def step(self, number, **kw):
+        self.tr.adamw_step(self.tensors, number, **kw)
+
+    def values(self, moment):
+        if self.scales is None:
+            return (self.m, self.v)[moment - 1].cpu().double().numpy()
+        out = torch.full((self.p.numel(),), float("nan"), device="cuda")
+        self.tr.adamw_state_values((self.m, self.v)[moment - 1], self.scales[moment - 1], out, moment)
+        return out.cpu().double().numpy()
+
+
+@pytest.mark.parametrize("size", [1e-9, 1e-11, 3e-12, 1e-13, 1e-14, 1e-16, 1e-18, 1e-20, 1e-25, 1e-37])
+def test_codes_of_tiny_runs(tr, size):
+    """Whatever a run's largest value is, it has the top level, and each code is the level whose thresholds the value lies
+    between. Values whose root is held with n bits below f32's smallest normal one carry that rounding, and no more."""
+    say(f"case adamw gradients of {size}")
+    gen = np.random.default_rng(3)
+    n, beta1, beta2 = 1000, 0.9, 0.95
+    g = (gen.normal(size=n) * 10.0 ** gen.uniform(-2, 0, n) * size).astype(np.float32)
+    for offset in (0, 1):                          # whole vectors, and element by element
+        buf = torch.zeros(n + 1, device="cuda")
+        buf[offset:offset + n] = torch.from_numpy(g).cuda()
+        t = State(tr, buf[offset:offset + n], 8)
+        t.step(1, lr=1e-3, beta1=beta1, beta2=beta2, eps=1e-8)
+        g64 = g.astype(np.float64)
+        for k, (exact, levels, power) in enumerate([((1 - beta1) * g64, 127, 2), ((1 - beta2) * g64 * g64, 255, 4)]):
+            e = 8 * ref.U * np.abs(exact) + 2 * LEAST      # 1 - beta, the products and the sum
+            scale = t.scales[k].cpu().double().numpy()
+            top = ref.runs(np.abs(exact)).max(1)
+            assert np.all(np.abs(scale - top) <= ref.runs(e).max(1)), (k, scale, top)
+            code = (t.m, t.v)[k].cpu().numpy().astype(np.int64)
+            level = code & 127 if k == 0 else code
+            s = np.repeat(scale, 256)[:n]
+            assert np.all(ref.runs(level).max(1)[scale > 0] == levels), (k, ref.runs(level).max(1))
+            low, high = s * (np.maximum(level - 0.5, 0) / levels) ** power, s * ((level + 0.5) / levels) ** power
+            slip = e + 8 * ref.U * np.abs(exact)
+            assert np.all((np.abs(exact) <= high + slip) | (level == levels)), f"moment {k + 1}: level too low"
+            assert np.all((np.abs(exact) >= low - slip) | ((level == 1) & (k == 1))), f"moment {k + 1}: level too high"
+            held = ref.values(code.astype(np.uint8), scale, k + 1)
+            got = t.values(k + 1)
+            assert np.all(np.abs(got - held) <= 4 * ref.U * np.abs(held) + LEAST), (k, got[:4], held[:4])
+
+
+@pytest.mark.parametrize("eps", [1e-12, 1e-15, 0.0])
+@pytest.mark.parametrize("size", [1e-3, 1e-12, 1e-13, 1e-15])
+def test_tiny_gradients_move_as_large_ones(tr, size, eps):
+    """Steps with gradients of one value: with any eps far below it an element moves by lr a step, in 8 bits as in 32."""
+    if eps > size * 1e-2:
+        pytest.skip("eps is no small part of the gradient")
+    say(f"case adamw 60 steps of {size}, eps {eps}")
+    for bits in (32, 8):
+        t = State(tr, torch.full((512,), size, device="cuda"), bits)
+        for k in range(60):
+            t.step(k + 1, lr=1e-3, beta1=0.9, beta2=0.95, eps=eps)
+        # the codes of a constant run are exact (the top level): what is left are some 10 roundings a step and eps' share
+        assert float((t.p + 0.06).abs().max()) <= 0.06 * (1000 * ref.U + 1.1 * eps / size), (bits, t.p[:4])
