@@ -44,11 +44,13 @@ constexpr int kStep = kThreads * kVec;
 constexpr int kSteps = 4;
 constexpr int kChunk = kSteps * kStep;         // elements of a workgroup
 static_assert(FP_ADAMW_BLOCK == 64 * kVec, "a run of shared scales is a wave's");
+static_assert(kVec == 4, "a thread's smallest v is taken of 4");
 constexpr int kTensors = 48;                   // of one launch
 // Runs whose scale is below kSmall are worked on times kLift, which is exact: the
 // reciprocals that lead to codes would overflow, and what one unit of a level
 // stands for would lose bits below the normal numbers.
-constexpr float kSmall = 0x1p-64f, kLift = 0x1p84f;
+constexpr float kSmall = 0x1p-64f, kLift = 0x1p84f, kRootLift = 0x1p-42f;   // the last: the root of 1 / kLift
+constexpr float kNormal = 0x1p-126f;
 constexpr float kNone = 0x1p-80f;              // below any other scale's reciprocal: for runs of zeros
 constexpr float kTopM = 127.f * 127.f, kTopV = 65025.f * 65025.f;   // 127^2, 255^4
 
@@ -211,6 +213,14 @@ struct Step {
       nv[e] = nv[e] * a.beta2 + ge * ge * a.om2;
       // the update is a small part of the parameter: the hardware's root and reciprocal (1 ulp) serve it
       rv[e] = __builtin_amdgcn_sqrtf(nv[e]);
+    }
+    // below the normal numbers that root is 0
+    if (fminf(fminf(nv[0], nv[1]), fminf(nv[2], nv[3])) < kNormal)
+#pragma unroll
+      for (int e = 0; e < kVec; ++e)
+        if (nv[e] < kNormal) rv[e] = __builtin_amdgcn_sqrtf(nv[e] * kLift) * kRootLift;
+#pragma unroll
+    for (int e = 0; e < kVec; ++e) {
       const float away = __builtin_fmaf(rv[e], a.far, a.eps);
       np[e] = __builtin_fmaf(p.a.get(e), keep, -(nm[e] * a.rate * __builtin_amdgcn_rcpf(away)));
       p.a.set(e, np[e]);
@@ -424,7 +434,8 @@ Rates rates_of(const fp_adamw_config* c) {
   r.beta1 = (float)c->beta1, r.om1 = (float)(1.0 - c->beta1), r.beta2 = (float)c->beta2, r.om2 = (float)(1.0 - c->beta2);
   r.rate = (float)(c->lr / (1.0 - std::pow(c->beta1, (double)c->step)));
   r.far = (float)(1.0 / std::sqrt(1.0 - std::pow(c->beta2, (double)c->step)));
-  r.eps = (float)c->eps;
+  // the hardware's reciprocal of what is below the normal numbers is infinite, and 0 times that no number
+  r.eps = c->eps > 0 ? std::max((float)c->eps, kNormal) : 0.f;
   r.copy_type = c->copy_type;
   return r;
 }

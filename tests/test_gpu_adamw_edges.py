@@ -1,4 +1,5 @@
-"""AdamW's states at the ends of f32's range: runs of 8-bit states whose largest value is tiny."""
+"""AdamW's states at the ends of f32's range: runs of 8-bit states whose largest value is tiny, roots below the normal numbers,
+gradients that are not finite."""
 
 import numpy as np
 import pytest
@@ -88,3 +89,22 @@ def test_tiny_gradients_move_as_large_ones(tr, size, eps):
             t.step(k + 1, lr=1e-3, beta1=0.9, beta2=0.95, eps=eps)
         # the codes of a constant run are exact (the top level): what is left are some 10 roundings a step and eps' share
         assert float((t.p + 0.06).abs().max()) <= 0.06 * (1000 * ref.U + 1.1 * eps / size), (bits, t.p[:4])
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_root_of_a_state_below_the_normal_numbers(tr, bits):
+    """v of 5e-44 is 36 times the smallest f32, so its root is known to 1 / 72: the step is finite and lr to that accuracy."""
+    say(f"case adamw v below 2^-126, {bits} bits")
+    t = State(tr, torch.full((300,), 1e-21, device="cuda"), bits)
+    t.step(1, lr=1e-3, beta1=0.9, beta2=0.95, eps=0.0)
+    assert float((t.p + 1e-3).abs().max()) <= 1e-3 * 0.02, t.p[:4]
+
+
+@pytest.mark.parametrize("eps", [1e-38, 1e-40, 1e-60])
+def test_eps_below_the_normal_numbers(tr, eps):
+    """Above 0 it keeps elements without a gradient where they are."""
+    say(f"case adamw eps {eps}")
+    for bits in (32, 8):
+        t = State(tr, torch.zeros(300, device="cuda"), bits, 0.5)
+        t.step(1, lr=1e-3, eps=eps)
+        assert bool((t.p == 0.5).all()), (bits, t.p[:4])
