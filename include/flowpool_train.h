@@ -163,7 +163,8 @@ fp_status vocab_loss_backward(const void* x, int64_t x_stride, const void* weigh
  * and scales are the state before the first step. The step itself is computed
  * in f32 before the new state is rounded.
  * Gradients have to be finite: a NaN or infinity reaches its element's
- * parameter and state, and with 8 bits the run's scale. */
+ * parameter (as NaN) and state, and with 8 bits the run's scale, which is then
+ * the NaN or infinity and makes all of the run's parameters NaN a step later. */
 #define FP_ADAMW_BLOCK 256
 
 typedef struct fp_adamw_tensor {

@@ -44,7 +44,7 @@ constexpr int kStep = kThreads * kVec;
 constexpr int kSteps = 4;
 constexpr int kChunk = kSteps * kStep;         // elements of a workgroup
 static_assert(FP_ADAMW_BLOCK == 64 * kVec, "a run of shared scales is a wave's");
-static_assert(kVec == 4, "a thread's smallest v is taken of 4");
+static_assert(kVec == 4, "a thread's smallest v, and whether any value is NaN, are taken of 4");
 constexpr int kTensors = 48;                   // of one launch
 // Runs whose scale is below kSmall are worked on times kLift, which is exact: the
 // reciprocals that lead to codes would overflow, and what one unit of a level
@@ -134,7 +134,9 @@ __device__ __forceinline__ float above(float c) { return c * (c + 1.f) + 0.25f; 
 // The level of t, given its root to within 8 units of its last place: the
 // largest c with t at or above c - 1/2 to the same power. The root less kLow
 // leads to it or to the one below it, so one comparison decides (NaN: level 0).
-// t is at most the top level's by two roundings, so no level is above that.
+// t is at most the top level's by two roundings, so no level is above that. A
+// run that holds a NaN has a NaN for its scale, and one that holds an infinity
+// that: their levels are 0.
 constexpr float kLow = 0x1p-12f;               // 16 units of the last place of 255
 // t = |m| 127^2 / scale, r its square root.
 __device__ __forceinline__ uint32_t level_m(float t, float r) {
@@ -246,6 +248,9 @@ struct Step {
       }
       hm = reduce64<Max>(hm);
       hv = reduce64<Max>(hv);
+      // a maximum passes over a NaN
+      if (__ballot(__builtin_isunordered(nm[0], nm[1]) | __builtin_isunordered(nm[2], nm[3]))) hm = __builtin_nanf("");
+      if (__ballot(__builtin_isunordered(nv[0], nv[1]) | __builtin_isunordered(nv[2], nv[3]))) hv = __builtin_nanf("");
       float lm = hm, lv = hv;                    // what the codes are made against
       if (hm < kSmall) {
         lm *= kLift;
@@ -260,7 +265,8 @@ struct Step {
           rv[e] = __builtin_amdgcn_sqrtf(nv[e]);
         }
       }
-      const float im = 1.f / fmaxf(lm, kNone) * kTopM, iv = 1.f / fmaxf(lv, kNone) * kTopV;
+      // (a NaN stays one)
+      const float im = 1.f / (lm < kNone ? kNone : lm) * kTopM, iv = 1.f / (lv < kNone ? kNone : lv) * kTopV;
       const float riv = __builtin_amdgcn_sqrtf(iv);
 #pragma unroll
       for (int e = 0; e < kVec; ++e) {

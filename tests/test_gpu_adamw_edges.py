@@ -108,3 +108,42 @@ def test_eps_below_the_normal_numbers(tr, eps):
         t = State(tr, torch.zeros(300, device="cuda"), bits, 0.5)
         t.step(1, lr=1e-3, eps=eps)
         assert bool((t.p == 0.5).all()), (bits, t.p[:4])
+
+
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), float("-inf")])
+@pytest.mark.parametrize("offset", [0, 1])
+def test_gradient_that_is_not_finite(tr, bad, offset):
+    """It reaches its element's parameter and state, in 8 bits its run's scales, and with them the run's next step; nothing
+    else."""
+    say(f"case adamw gradient {bad} offset {offset}")
+    n, at = 5000, 1300
+    run = slice(1280, 1536)
+    for bits in (32, 8):
+        buf = torch.linspace(-1, 1, n + 1, device="cuda")
+        t = State(tr, buf[offset:offset + n], bits, 0.5)
+        good = State(tr, t.g.clone(), bits, 0.5)
+        t.g[at] = bad
+        for s in (t, good):
+            s.step(1, lr=1e-3)
+        others = torch.arange(n, device="cuda") != at
+        assert bool(torch.isnan(t.p[at])) and torch.equal(t.p[others], good.p[others])
+        if bits == 32:
+            want = [bad, abs(bad)]
+            for state, clean, w in ((t.m, good.m, want[0]), (t.v, good.v, want[1])):
+                assert np.isnan(w) and bool(torch.isnan(state[at])) or float(state[at]) == w
+                assert torch.equal(state[others], clean[others])
+            continue
+        runs = torch.arange(t.scales.shape[1], device="cuda") != at // 256
+        for k in (0, 1):
+            top = float(t.scales[k, at // 256])
+            assert np.isnan(top) if np.isnan(bad) else top == float("inf"), top
+            assert torch.equal(t.scales[k][runs], good.scales[k][runs])
+        assert bool((t.m[run] % 128 == 0).all()) and bool((t.v[run] <= 1).all())       # v above 0 has no level 0
+        outside = torch.ones(n, dtype=torch.bool, device="cuda")
+        outside[run] = False
+        assert torch.equal(t.m[outside], good.m[outside]) and torch.equal(t.v[outside], good.v[outside])
+        t.g[at] = 0.0
+        good.g[at] = 0.0
+        for s in (t, good):
+            s.step(2, lr=1e-3)
+        assert bool(torch.isnan(t.p[run]).all()) and torch.equal(t.p[outside], good.p[outside])
