@@ -39,8 +39,15 @@ def next_ids(spec: SampleSpec) -> np.ndarray:
     return np.append(rows[1:], NO_LABEL).astype(np.int32)
 
 
+def clip_factor(grads, clip: float):
+    """The factor that brings the gradients' norm down to `clip`, f32 [1]. Where the norm is not finite neither is the factor,
+    and adamw_step changes nothing (clip over an infinite norm would be 0, a step like any other)."""
+    norm = torch.sqrt(sum(g.square().sum() for g in grads))
+    return torch.where(torch.isfinite(norm), torch.clamp(clip / norm, max=1.0), norm).reshape(1)
+
+
 class Model:
-    """f32 parameters, their bf16 copies and f32 gradients."""
+    """f32 parameters, their bf16 copies, f32 gradients and AdamW's states."""
 
     def __init__(self, hidden: int, vocab: int, seed: int):
         gen = torch.Generator(device="cuda").manual_seed(seed)
@@ -58,6 +65,7 @@ class Model:
         codes = [torch.zeros(n, dtype=torch.uint8, device="cuda") for _ in range(2)]
         scales = torch.zeros(2, -(-n // tr.FP_ADAMW_BLOCK), device="cuda")
         flat = lambda d: [d["head"].view(-1)]  # noqa: E731
+        self.states = [*zeros[0], *zeros[1], *codes, scales]
         self.head = tr.adamw_tensors(flat(self.params), flat(self.grads), codes[:1], codes[1:], scales=[scales],
                                      copies=flat(self.bf16), weight_decay=0.01)
 
@@ -103,12 +111,15 @@ class Trainer:
             tr.norm_backward(dy, z, m.bf16["weight"], mean, rstd, dz, m.grads["weight"], m.grads["bias"], self.space,
                              accumulate=True)
             m.grads["adapter"] += x.t() @ dz
-        norm = torch.sqrt(sum(g.square().sum() for g in m.grads.values()))
-        scale = torch.clamp(clip / norm, max=1.0).reshape(1)             # NaN or infinity: the step changes nothing
-        self.steps += 1
-        for group in (m.inner, m.head):
-            tr.adamw_step(group, self.steps, lr, 0.9, 0.95, grad_scale=scale)
+        self.update(lr, clip)
         return float(total) / n_labelled
+
+    def update(self, lr: float, clip: float) -> None:
+        """One AdamW step of the model's gradients."""
+        scale = clip_factor(self.model.grads.values(), clip)
+        self.steps += 1
+        for group in (self.model.inner, self.model.head):
+            tr.adamw_step(group, self.steps, lr, 0.9, 0.95, grad_scale=scale)
 
     def close(self):
         self.work.close()
