@@ -6,7 +6,8 @@ nothing) and checks what a kernel could not: shapes, types, devices and
 strides. Streams are given as in ``paper_2606_23087_amd.flowpool``: a torch
 stream, a raw hipStream_t, or None for torch's current stream. As there, a
 tensor that another stream still uses has to be kept alive and ordered by the
-caller. A non-OK status raises ``FlowPoolError``.
+caller. The tensors have to be on the current device. A non-OK status raises
+``FlowPoolError``.
 
     workspace = torch.empty(vocab_loss_workspace(rows, hidden, vocab), dtype=torch.uint8, device="cuda")
     vocab_loss_forward(x, weight, labels, loss, lse, None, workspace)
@@ -75,6 +76,18 @@ def _device(x: torch.Tensor, name: str):
 def _on(x: torch.Tensor, name: str, device) -> None:
     if x.device != device:
         raise ValueError(f"{name} is on {x.device}, the call's other tensors on {device}")
+
+
+def _queue(stream, device):
+    """The stream of a call on tensors of `device`, which has to be the current one: the library launches there."""
+    here = torch._C._cuda_getDevice()
+    if device.index != here:
+        raise ValueError(f"the tensors are on {device}, the current device is {here}")
+    if stream is None:
+        return torch._C._cuda_getCurrentRawStream(here)
+    if isinstance(stream, torch.cuda.Stream) and stream.device != device:
+        raise ValueError(f"stream is of {stream.device}, the tensors are on {device}")
+    return _stream(stream)
 
 
 def _matrix(x: torch.Tensor, name: str, device, dtype=None, shape=None) -> int:
@@ -147,7 +160,7 @@ def norm_forward(x, weight, bias, y, mean, rstd, eps: float = 1e-5, stream=None)
     w, b, wtype = _weights(weight, bias, dev, x.dtype, hidden)
     f32 = (torch.float32,)
     _check(_lib.norm_forward(x.data_ptr(), xs, w, b, y.data_ptr(), ys, _vector(mean, "mean", dev, f32, rows),
-                             _vector(rstd, "rstd", dev, f32, rows), rows, hidden, eps, TYPES[x.dtype], wtype, _stream(stream)),
+                             _vector(rstd, "rstd", dev, f32, rows), rows, hidden, eps, TYPES[x.dtype], wtype, _queue(stream, dev)),
            "norm_forward")
 
 
@@ -170,7 +183,7 @@ def norm_backward(dy, x, weight, mean, rstd, dx, dweight, dbias, workspace, accu
     _check(_lib.norm_backward(dy.data_ptr(), gs, x.data_ptr(), xs, w, _vector(mean, "mean", dev, f32, rows),
                               _vector(rstd, "rstd", dev, f32, rows), dx.data_ptr(), ds, _vector(dweight, "dweight", dev, f32, hidden),
                               _vector(dbias, "dbias", dev, f32, hidden), rows, hidden, TYPES[x.dtype], wtype, int(accumulate),
-                              room, size, _stream(stream)), "norm_backward")
+                              room, size, _queue(stream, dev)), "norm_backward")
 
 
 # ------------------------------------------------------------------ vocabulary loss
@@ -197,7 +210,7 @@ def vocab_loss_forward(x, weight, labels, loss, lse, n_labelled, workspace, redu
     room, size = _room(workspace, dev)
     _check(_lib.vocab_loss_forward(xp, xs, wp, ws, lab, x.shape[0], x.shape[1], weight.shape[0], TYPES[x.dtype],
                                    REDUCTIONS[reduction], _vector(loss, "loss", dev, (torch.float32,), 1), lsep,
-                                   _vector(n_labelled, "n_labelled", dev, (torch.int32,), 1), room, size, _stream(stream)),
+                                   _vector(n_labelled, "n_labelled", dev, (torch.int32,), 1), room, size, _queue(stream, dev)),
            "vocab_loss_forward")
 
 
@@ -216,7 +229,7 @@ def vocab_loss_backward(x, weight, labels, lse, dloss, dx, dweight, workspace, r
                                     dx.data_ptr() if dx is not None else None, dxs,
                                     dweight.data_ptr() if dweight is not None else None, dws,
                                     TYPES[dweight.dtype] if dweight is not None else TYPES[x.dtype], int(accumulate), room, size,
-                                    _stream(stream)), "vocab_loss_backward")
+                                    _queue(stream, dev)), "vocab_loss_backward")
 
 
 # ------------------------------------------------------------------ AdamW
@@ -294,7 +307,10 @@ def adamw_step(tensors: AdamwTensors, step: int, lr: float, beta1: float = 0.9, 
     if tensors.table is None:
         _check(_lib.adamw_step(tensors.array, tensors.n, C.byref(config), scale, _stream(stream)), "adamw_step")
     else:
-        _check(_lib.adamw_table_step(tensors.table.data_ptr(), tensors.groups, C.byref(config), scale, _stream(stream)),
+        if grad_scale is not None:
+            _on(grad_scale, "grad_scale", tensors.table.device)
+        _check(_lib.adamw_table_step(tensors.table.data_ptr(), tensors.groups, C.byref(config), scale,
+                                     _queue(stream, tensors.table.device)),
                "adamw_table_step")
 
 
@@ -304,5 +320,5 @@ def adamw_state_values(codes, scales, out, moment: int, stream=None) -> None:
     n = codes.numel()
     _check(_lib.adamw_state_values(_vector(codes, "codes", dev, (torch.uint8,), n),
                                    _vector(scales, "scales", dev, (torch.float32,), -(-n // FP_ADAMW_BLOCK)),
-                                   _vector(out, "out", dev, (torch.float32,), n), n, moment, _stream(stream)),
+                                   _vector(out, "out", dev, (torch.float32,), n), n, moment, _queue(stream, dev)),
            "adamw_state_values")
