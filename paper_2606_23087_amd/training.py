@@ -236,11 +236,12 @@ def vocab_loss_backward(x, weight, labels, lse, dloss, dx, dweight, workspace, r
 
 class AdamwTensors:
     """The tensors of an optimizer, checked and listed once (``adamw_tensors``): it keeps them alive, and their table on
-    the GPU."""
+    the GPU. It may be dropped while a step is queued, on any stream; a captured step needs it for as long as its graph is
+    replayed."""
 
     def __init__(self, array, n, types, held, device):
         self.array, self.n, self.types, self._held = array, n, types, held
-        self.table, self.groups = None, 0
+        self.table, self.groups, self._streams = None, 0, set()
         if device is not None:
             self.table = torch.empty(_bytes(_lib.adamw_table_bytes(n), "adamw_table_bytes"), dtype=torch.uint8, device=device)
             groups = C.c_int64()
@@ -249,6 +250,17 @@ class AdamwTensors:
                                               self.table.nbytes, C.byref(groups), _stream(None)), "adamw_table_write")
                 torch.cuda.current_stream().synchronize()       # steps may run on any stream
             self.groups = groups.value
+            self._streams.add(torch.cuda.current_stream(device).cuda_stream)
+
+    def used_on(self, stream: int) -> None:
+        """Tells the allocator that the step's stream uses what the step reads by address alone: a tensor that is freed goes
+        to its own stream's next allocation, whatever another one still has queued."""
+        if stream not in self._streams:
+            device = self.table.device
+            torch_stream = torch.cuda.ExternalStream(stream, device) if stream else torch.cuda.default_stream(device)
+            for t in (self.table, *(t for group in self._held if group is not None for t in group)):
+                t.record_stream(torch_stream)
+            self._streams.add(stream)
 
 
 def _one_type(tensors, name, allowed):
@@ -309,8 +321,9 @@ def adamw_step(tensors: AdamwTensors, step: int, lr: float, beta1: float = 0.9, 
     else:
         if grad_scale is not None:
             _on(grad_scale, "grad_scale", tensors.table.device)
-        _check(_lib.adamw_table_step(tensors.table.data_ptr(), tensors.groups, C.byref(config), scale,
-                                     _queue(stream, tensors.table.device)),
+        queue = _queue(stream, tensors.table.device)
+        tensors.used_on(queue)
+        _check(_lib.adamw_table_step(tensors.table.data_ptr(), tensors.groups, C.byref(config), scale, queue),
                "adamw_table_step")
 
 

@@ -85,3 +85,27 @@ def test_grad_scale_of_another_device(tr):
 
     with pytest.raises(ValueError, match="grad_scale"):
         tr.adamw_step(o.tensors, 1, 1e-3, grad_scale=Elsewhere())
+
+
+def test_list_of_tensors_dropped_behind_a_queued_step(tr):
+    """A step queued on another stream reads its table and its tensors by address: once the list of them is dropped, nothing may
+    be given their memory before the step has run."""
+    n = 300000
+    for raw in (False, True):
+        side = torch.cuda.Stream()
+        p, g, m, v = (torch.full((n,), 1.0, device="cuda") for _ in range(4))
+        tensors = tr.adamw_tensors([p], [g], [m], [v])
+        want = p.clone(), g.clone(), m.clone(), v.clone()
+        tr.adamw_step(tr.adamw_tensors(*[[t] for t in want]), 1, 1e-3)
+        size, taken = tensors.table.nbytes, {tensors.table.data_ptr(), g.data_ptr(), v.data_ptr()}
+        torch.cuda.synchronize()
+        with torch.cuda.stream(side):
+            torch.cuda._sleep(2_000_000_000)
+        tr.adamw_step(tensors, 1, 1e-3, stream=side.cuda_stream if raw else side)
+        del tensors, g, v
+        after = [torch.zeros(size, dtype=torch.uint8, device="cuda"), *(torch.zeros(n, device="cuda") for _ in range(6))]
+        queued = not side.query()
+        assert taken.isdisjoint(t.data_ptr() for t in after)
+        torch.cuda.synchronize()
+        assert queued, "the step was over before memory was asked for: the test shows nothing"
+        assert torch.equal(p, want[0]) and torch.equal(m, want[2]) and all(bool((t == 0).all()) for t in after)
