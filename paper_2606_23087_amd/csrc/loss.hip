@@ -120,22 +120,27 @@ struct Classes {
 };
 
 // Orders the rows of the `tile`-th 256 classes: a stable counting sort, whose
-// place among all classes is the number of rows below the tile. Each of 4 waves
-// has a quarter of the rows, in their order.
+// place among all classes is the number of rows below the tile. Each of 16 waves
+// has a 16th of the rows, in their order, and loads 8 of a lane at once: few
+// classes are few workgroups, whose time is a wave's chain of steps (32768 rows
+// over 1000 classes: 100 us with 4 waves).
+constexpr int kOrderWaves = 16;
 __device__ __forceinline__ void order_classes(const Classes& o, int32_t tile, const int32_t* picks, int32_t n, int32_t vocab) {
-  __shared__ int32_t at[4][256], first[256], total[256], sums[8];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  constexpr int kAtOnce = 8;
+  __shared__ int32_t at[kOrderWaves][256], first[256], total[256], sums[kOrderWaves], ends[4];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c0 = threadIdx.x;
 #pragma unroll
-  for (int w = 0; w < 4; ++w) at[w][threadIdx.x] = 0;
+  for (int k = 0; k < kOrderWaves * 256; k += kOrderWaves * 64) (&at[0][0])[k + threadIdx.x] = 0;
   __syncthreads();
-  const int32_t quarter = (n + 255) / 256 * 64, from = min(wave * quarter, n), to = min(from + quarter, n), v0 = tile * 256;
+  const int32_t share = (n + kOrderWaves * 64 - 1) / (kOrderWaves * 64) * 64, from = min(wave * share, n), to = min(from + share, n);
+  const int32_t v0 = tile * 256;
   int32_t below = 0;
-  for (int32_t i = from + lane; i < to; i += 256) {
-    int32_t c[4];
+  for (int32_t i = from + lane; i < to; i += 64 * kAtOnce) {
+    int32_t c[kAtOnce];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) c[e] = i + 64 * e < to ? picks[i + 64 * e] - v0 : 256;
+    for (int e = 0; e < kAtOnce; ++e) c[e] = i + 64 * e < to ? picks[i + 64 * e] - v0 : 256;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
+    for (int e = 0; e < kAtOnce; ++e) {
       below += c[e] < 0;
       if ((uint32_t)c[e] < 256u) atomicAdd(&at[wave][c[e]], 1);
     }
@@ -144,37 +149,43 @@ __device__ __forceinline__ void order_classes(const Classes& o, int32_t tile, co
   for (int d = 1; d < 64; d *= 2) below += __shfl_xor(below, d);
   if (lane == 0) sums[wave] = below;
   __syncthreads();
-  int32_t mine = 0;
+  int32_t mine = 0, before = 0;                  // rows of class c0; of it and the wave's classes before it
+  if (c0 < 256) {
 #pragma unroll
-  for (int w = 0; w < 4; ++w) mine += at[w][threadIdx.x];
-  int32_t before = mine;                         // inclusive over the wave
+    for (int w = 0; w < kOrderWaves; ++w) mine += at[w][c0];
+    before = mine;
 #pragma unroll
-  for (int d = 1; d < 64; d *= 2) {
-    const int32_t o2 = __shfl_up(before, d);
-    if (lane >= d) before += o2;
-  }
-  if (lane == 63) sums[4 + wave] = before;
-  __syncthreads();
-  int32_t place = before - mine + sums[0] + sums[1] + sums[2] + sums[3];
-#pragma unroll
-  for (int w = 0; w < 4; ++w)
-    if (w < wave) place += sums[4 + w];
-  first[threadIdx.x] = place;
-  total[threadIdx.x] = mine;
-  if (v0 + (int)threadIdx.x < vocab) o.begin[v0 + threadIdx.x] = mine ? place : -1;
-#pragma unroll
-  for (int w = 0; w < 4; ++w) {
-    const int32_t here = at[w][threadIdx.x];
-    at[w][threadIdx.x] = place;
-    place += here;
+    for (int d = 1; d < 64; d *= 2) {
+      const int32_t other = __shfl_up(before, d);
+      if (lane >= d) before += other;
+    }
+    if (lane == 63) ends[wave] = before;
   }
   __syncthreads();
-  for (int32_t base = from; base < to; base += 256) {
-    int32_t c[4];
+  if (c0 < 256) {
+    int32_t place = before - mine;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) c[e] = base + 64 * e + lane < to ? picks[base + 64 * e + lane] - v0 : 256;
+    for (int w = 0; w < kOrderWaves; ++w) place += sums[w];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
+    for (int w = 0; w < 4; ++w)
+      if (w < wave) place += ends[w];
+    first[c0] = place;
+    total[c0] = mine;
+    if (v0 + c0 < vocab) o.begin[v0 + c0] = mine ? place : -1;
+#pragma unroll
+    for (int w = 0; w < kOrderWaves; ++w) {
+      const int32_t here = at[w][c0];
+      at[w][c0] = place;
+      place += here;
+    }
+  }
+  __syncthreads();
+  for (int32_t base = from; base < to; base += 64 * kAtOnce) {
+    int32_t c[kAtOnce];
+#pragma unroll
+    for (int e = 0; e < kAtOnce; ++e) c[e] = base + 64 * e + lane < to ? picks[base + 64 * e + lane] - v0 : 256;
+#pragma unroll
+    for (int e = 0; e < kAtOnce; ++e) {
       const bool in = (uint32_t)c[e] < 256u;
       uint64_t same = __ballot(in);              // lanes with this lane's class
       if (!same) continue;
@@ -199,19 +210,20 @@ __device__ __forceinline__ void order_classes(const Classes& o, int32_t tile, co
 
 // Gathers the labelled rows into xc [.., ld], zeros from hidden to ld, and with
 // them (backward) their lse. Past the last row nothing is written: those rows
-// of a tile are read as the last one, and left out of every result. Workgroups
-// past the n_rows-th order the rows by class, a tile of classes each.
+// of a tile are read as the last one, and left out of every result. A workgroup
+// has 4 rows, 256 threads each; the first `tiles` order the rows by class, a tile
+// of classes each.
 template <class T>
-__global__ __launch_bounds__(256) void k_gather_rows(const T* x, int64_t x_stride, const int32_t* rows, const int32_t* count,
-                                                     int32_t hidden, int32_t ld, T* xc, const float* lse, float* lses, int32_t n_rows,
-                                                     const int32_t* picks, int32_t vocab, Classes classes) {
-  const int32_t i = blockIdx.x;
-  if (i >= n_rows) return order_classes(classes, i - n_rows, picks, *count, vocab);
+__global__ __launch_bounds__(1024) void k_gather_rows(const T* x, int64_t x_stride, const int32_t* rows, const int32_t* count,
+                                                      int32_t hidden, int32_t ld, T* xc, const float* lse, float* lses, int32_t tiles,
+                                                      const int32_t* picks, int32_t vocab, Classes classes) {
+  if ((int32_t)blockIdx.x < tiles) return order_classes(classes, blockIdx.x, picks, *count, vocab);
+  const int32_t i = (blockIdx.x - tiles) * 4 + (threadIdx.x >> 8), t = threadIdx.x & 255;
   if (i >= *count) return;
-  if (lse && threadIdx.x == 0) lses[i] = lse[rows[i]];
+  if (lse && t == 0) lses[i] = lse[rows[i]];
   const T* src = x + (int64_t)rows[i] * x_stride;
   T* dst = xc + (int64_t)i * ld;
-  for (int32_t c = threadIdx.x * 8; c < ld; c += 256 * 8) {
+  for (int32_t c = t * 8; c < ld; c += 256 * 8) {
     u32x4 v = {0, 0, 0, 0};
     if (c < hidden) v = *(const u32x4*)(src + c);
     *(u32x4*)(dst + c) = v;
@@ -848,42 +860,90 @@ __device__ __forceinline__ void finish_row(const LossArgs& a, int32_t t, int32_t
   }
 }
 
+// Adds up the rows at places `from` to `to` of the order, each times its gradient
+// at the label, 8 columns a lane from c on: every fourth row, 8 under way.
+template <class T>
+__device__ __forceinline__ void add_rows(const LossArgs& a, const Classes& o, int32_t from, int32_t to, int32_t c, float (&s)[8]) {
+  for (int32_t k = from + uniform(threadIdx.x >> 6); k < to; k += 32) {
+    int32_t row[8];
+    float own[8];
+    Pack<T, 8> x[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) row[e] = o.order[min(k + 4 * e, to - 1)];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      own[e] = k + 4 * e < to ? a.own[row[e]] : 0.f;
+      x[e] = load<T, 8>((const T*)a.xc + (int64_t)row[e] * a.ld + c);
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (k + 4 * e < to)
+#pragma unroll
+        for (int d = 0; d < 8; ++d) s[d] += own[e] * x[e].get(d);
+  }
+}
+// Adds the 4 waves' sums to the first one's, in order. All of the workgroup.
+__device__ __forceinline__ void join_waves(float (&s)[8], float (*parts)[8][64]) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  if (wave)
+#pragma unroll
+    for (int d = 0; d < 8; ++d) parts[wave - 1][d][lane] = s[d];
+  __syncthreads();
+  if (!wave)
+#pragma unroll
+    for (int d = 0; d < 8; ++d) s[d] = ((s[d] + parts[0][d][lane]) + parts[1][d][lane]) + parts[2][d][lane];
+  __syncthreads();
+}
+
+// A class that many rows share is added up by more than one workgroup: the sums
+// of each kPart places that are all its own (the order is by class, so the first
+// and the last tell) wait in the side row of the second place, which no class
+// begins at. Without this 32768 rows of one class take 3.4 ms over 1000 x 1024,
+// with it 0.95, as rows of different classes do.
+constexpr int32_t kPart = 256;
+template <class T>
+__global__ __launch_bounds__(256) void k_class_parts(LossArgs a, Classes o) {
+  __shared__ float parts[3][8][64];
+  const int32_t i = blockIdx.x * kPart;
+  if (i + kPart > *a.count || a.picks[o.order[i]] != a.picks[o.order[i + kPart - 1]]) return;
+  const int32_t c = blockIdx.y * 512 + (threadIdx.x & 63) * 8;
+  float s[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+  add_rows<T>(a, o, i, i + kPart, min(c, a.hidden - 8), s);
+  join_waves(s, parts);
+  if (threadIdx.x < 64 && c < a.hidden) {
+    Pack<float, 8> p;
+#pragma unroll
+    for (int d = 0; d < 8; ++d) p.set(d, s[d]);
+    store<float, 8>(a.side + (int64_t)(i + 1) * a.ld + c, p);
+  }
+}
+
 // The row of dweight of the class whose rows begin at place i: its sums over the
 // piece's product, and each of its own rows times that row's gradient at the
-// label. 512 columns at a time; each of 4 waves adds up every fourth row, 8 under
-// way, and the first one joins them.
+// label. 512 columns at a time.
 template <class T, class O>
 __device__ __forceinline__ void finish_class(const LossArgs& a, const Classes& o, int32_t i, float f, O* dweight, int64_t dw_ld,
-                                             int32_t add) {
+                                             int32_t add, bool in_parts) {
   __shared__ float parts[3][8][64];
   const int32_t many = uniform(o.many[i]);
   if (!many) return;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int64_t v = a.picks[o.order[i]];
+  // places up to the first whole part, whole parts, and places behind the last; without whole parts all are the first
+  int32_t whole = (i + kPart - 1) / kPart, end = (i + many) / kPart;
+  if (!in_parts || whole >= end) whole = end = (i + many + kPart - 1) / kPart;
   for (int32_t c0 = blockIdx.y * 2048; c0 < min(a.hidden, (int32_t)(blockIdx.y + 1) * 2048); c0 += 512) {
     const int32_t c = c0 + lane * 8, at = min(c, a.hidden - 8);
     float s[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-    for (int32_t k = wave; k < many; k += 32) {
-      int32_t row[8];
-      float own[8];
-      Pack<T, 8> x[8];
+    add_rows<T>(a, o, i, min(whole * kPart, i + many), at, s);
+#pragma unroll 8
+    for (int32_t k = whole + wave; k < end; k += 4) {
+      const Pack<float, 8> p = load<float, 8>(a.side + (int64_t)(k * kPart + 1) * a.ld + at);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) row[e] = o.order[i + min(k + 4 * e, many - 1)];
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        own[e] = k + 4 * e < many ? a.own[row[e]] : 0.f;
-        x[e] = load<T, 8>((const T*)a.xc + (int64_t)row[e] * a.ld + at);
-      }
-#pragma unroll
-      for (int e = 0; e < 8; ++e)
-        if (k + 4 * e < many)
-#pragma unroll
-          for (int d = 0; d < 8; ++d) s[d] += own[e] * x[e].get(d);
+      for (int d = 0; d < 8; ++d) s[d] += p.get(d);
     }
-    if (wave)
-#pragma unroll
-      for (int d = 0; d < 8; ++d) parts[wave - 1][d][lane] = s[d];
-    __syncthreads();
+    add_rows<T>(a, o, min(end * kPart, i + many), i + many, at, s);
+    join_waves(s, parts);
     if (!wave && c < a.hidden) {
       const Pack<float, 8> p = load<float, 8>(a.side + (int64_t)i * a.ld + c);
       O* const to = dweight + v * dw_ld + c;
@@ -893,10 +953,9 @@ __device__ __forceinline__ void finish_class(const LossArgs& a, const Classes& o
         if (add) old = load<float, 8>(to);
 #pragma unroll
       for (int d = 0; d < 8; ++d)
-        out.set(d, old.get(d) + f * (p.get(d) + (((s[d] + parts[0][d][lane]) + parts[1][d][lane]) + parts[2][d][lane])));
+        out.set(d, old.get(d) + f * (p.get(d) + s[d]));
       store<O, 8>(to, out);
     }
-    __syncthreads();
   }
 }
 
@@ -904,12 +963,12 @@ __device__ __forceinline__ void finish_class(const LossArgs& a, const Classes& o
 // behind a place in the order of the labelled rows.
 template <class T, class O>
 __global__ __launch_bounds__(256) void k_finish(LossArgs a, Classes o, const int32_t* slot, const float* dloss, int32_t mean, int32_t dx_rows,
-                                                T* dx, int64_t dx_stride, O* dweight, int64_t dw_ld, int32_t add) {
+                                                T* dx, int64_t dx_stride, O* dweight, int64_t dw_ld, int32_t add, int32_t in_parts) {
   const float f = factor<T>(dloss, a.count, mean);
   if ((int32_t)blockIdx.x < dx_rows)
     finish_row(a, blockIdx.x, slot[blockIdx.x], f, dx, dx_stride);
   else if ((int32_t)blockIdx.x - dx_rows < *a.count)
-    finish_class<T>(a, o, blockIdx.x - dx_rows, f, dweight, dw_ld, add);
+    finish_class<T>(a, o, blockIdx.x - dx_rows, f, dweight, dw_ld, add, in_parts);
 }
 
 // ------------------------------------------------------------------ host
@@ -1000,10 +1059,11 @@ hipError_t begin(const Plan& p, char* ws, const void* x, int64_t x_stride, const
   int32_t* const list = (int32_t*)(ws + p.rows);
   hipError_t e = launch(k_label_rows, dim3(1), dim3(1024), 0, s, labels, (int32_t)rows, vocab, list, (int32_t*)(ws + p.picks), slot,
                         count, count_out, zero_lse, (u32x4*)(ws + p.zeros));
-  const int64_t groups = rows + (classes.order ? (vocab + 255) / 256 : 0);
+  const int32_t tiles = classes.order ? (vocab + 255) / 256 : 0;
+  const int64_t groups = tiles + (rows + 3) / 4;
   if (e == hipSuccess && groups)
-    e = launch(k_gather_rows<T>, dim3((unsigned)groups), dim3(256), 0, s, (const T*)x, x_stride, (const int32_t*)list,
-               (const int32_t*)count, hidden, p.ld, (T*)(ws + p.xc), lse, (float*)(ws + p.lses), (int32_t)rows,
+    e = launch(k_gather_rows<T>, dim3((unsigned)groups), dim3(64 * kOrderWaves), 0, s, (const T*)x, x_stride, (const int32_t*)list,
+               (const int32_t*)count, hidden, p.ld, (T*)(ws + p.xc), lse, (float*)(ws + p.lses), tiles,
                (const int32_t*)(ws + p.picks), vocab, classes);
   return e;
 }
@@ -1075,11 +1135,15 @@ hipError_t backward(const Plan& p, char* ws, const void* x, int64_t x_stride, co
   if (e == hipSuccess)
     e = launch(k_own_gradient, dim3((unsigned)((rows + 15) / 16)), dim3(1024), 0, s, (const float*)a.others, a.others_ld,
                (int32_t)(2 * tiles(vocab)), a.count, (float*)(ws + p.own));
+  // up to two parts of rows are soon added up by the workgroup that finishes the class
+  const bool in_parts = dweight && rows > 2 * kPart;
+  if (in_parts && e == hipSuccess)
+    e = launch(k_class_parts<T>, dim3((unsigned)(rows / kPart), (unsigned)((hidden + 511) / 512)), dim3(256), 0, s, a, classes);
   const auto finish = [&](auto* dw) {
     using O = std::remove_pointer_t<decltype(dw)>;
     const dim3 grid((unsigned)((dx ? rows : 0) + (dweight ? rows : 0)), (unsigned)((hidden + 2047) / 2048));
     return launch(k_finish<T, O>, grid, dim3(256), 0, s, a, classes, (const int32_t*)slot, dloss, mean, (int32_t)(dx ? rows : 0), (T*)dx,
-                  dx_stride, dw, dw_stride, (int32_t)add);
+                  dx_stride, dw, dw_stride, (int32_t)add, (int32_t)in_parts);
   };
   if (e == hipSuccess) e = dw_f32 ? finish((float*)dweight) : finish((T*)dweight);
   return e;

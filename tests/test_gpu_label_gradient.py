@@ -108,7 +108,8 @@ def test_weight_gradient_at_the_label_is_not_rounded(tr, dtype):
     assert float(over.max()) <= 0, float(over.max())
 
 
-@pytest.mark.parametrize("rows,vocab", [(600, 1), (600, 3), (3000, 700), (65, 100000), (5000, 40000)])
+@pytest.mark.parametrize("rows,vocab", [(600, 1), (600, 3), (3000, 700), (65, 100000), (5000, 40000), (1400, 1), (5000, 1), (9000, 2),
+                                        (6000, 30)])
 def test_rows_of_one_class_are_added_in_order(tr, rows, vocab):
     """Labels that many rows share, few share and none share: dweight against 64 bits, and the same bits every time."""
     from test_gpu_training import loss_case, run_loss
