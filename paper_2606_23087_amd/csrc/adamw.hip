@@ -7,7 +7,7 @@
 //
 // A launch takes up to kTensors tensors, listed in its arguments, or any number
 // listed in a table in device memory, and cuts each into chunks of kChunk
-// elements, a workgroup each. (290 tensors of 6400 elements on average took 63
+// elements, a workgroup each. (290 tensors of 6690 elements on average took 63
 // us in 7 launches of 9, most of it their latency.) A lane has 4
 // consecutive elements at a time, so a wave's accesses are whole lines in every
 // type, and a run of 256 elements that share 8-bit scales is one wave's: its
@@ -17,11 +17,11 @@
 // of each operand; 2 and 8 are slower), and all pass the caches by (plain loads or
 // stores are slower).
 //
-// Measured at 545 million values: f32 gradients and states with a bf16 copy 2.94
-// ms, 5.6 TB/s; bf16 gradients, 8-bit states and a copy 1.59 ms, 4.8 TB/s, where the
-// codes' arithmetic takes about as long as the bytes, and 0.45 and 0.47 ms for the
-// values of each state (a large copy's rate); 290 tensors of 6400 values on
-// average 15.2 us.
+// Measured at 545 million values: f32 gradients and states with a bf16 copy 2.91
+// ms, 5.6 TB/s; bf16 gradients, 8-bit states and a copy 1.59 ms, 5.5 TB/s, where the
+// 93 vector instructions of a value take every issue slot, and 0.46 ms for the
+// values of each state (a large copy's rate); 290 tensors of 6690 values on
+// average (707 chunks, 290 of them ragged) 15.4 us.
 //
 // The codes have to come out alike wherever they are computed from the same
 // inputs, so the state's arithmetic is separate multiplications and additions

@@ -27,12 +27,12 @@
 // labels, whose sums waited in f32 (a counting sort of the labelled rows says
 // which rows a class has).
 //
-// Measured (bf16): the loss of 4096 labelled rows over 152064 x 4096 3.93 ms, 1300
-// TFLOP/s; a step of 4096 over 152064 x 3584 14.4 ms, of 8192 over 128256 x 5120
-// 32.7 ms, 1240 and 1320 TFLOP/s of what is multiplied (the logits twice). A large
-// library product reaches 1340 to 1540 here. Bound by what the L2s feed to the
-// LDS, about 11 TB/s: with loads left out the loop runs at 1990 TFLOP/s, with half
-// of them in proportion; neither barriers nor LDS reads show.
+// Measured (bf16): the loss of 4096 labelled rows over 152064 x 4096 3.90 ms, 1310
+// TFLOP/s; a step of 4096 over 152064 x 3584 14.6 ms, of 8192 over 128256 x 5120
+// 33.3 ms, 1220 and 1290 TFLOP/s of what is multiplied (the logits twice). A large
+// library product reaches 1320 to 1520 here. The matrix cores work in 0.71 of the
+// cycles, at the 1.7 GHz that the power allows, while the L2s feed the LDS at 10
+// TB/s; with the loads left out the loop runs at 1690 to 2000 TFLOP/s.
 
 #include "gemm.h"
 

@@ -274,7 +274,8 @@ def adamw_tensors(params: Sequence, grads: Sequence, m: Sequence, v: Sequence, s
                   copies: Optional[Sequence] = None, weight_decay=0.0) -> AdamwTensors:
     """The tensors of adamw_step, in place: parameters (f32 or bf16), gradients, states m and v (f32, or uint8 with
     ``scales``: for each tensor f32 [2, ceil(n / 256)], m's and v's), 16-bit copies of f32 parameters, and weight decay (one
-    number, or one a tensor). All are contiguous."""
+    number, or one a tensor). All are contiguous. The list holds their addresses, and making it waits for the current stream
+    (0.73 ms in all for 290 tensors): gradients are best zeroed in place, for ones that are allocated anew need a new list."""
     params, grads, m, v = list(params), list(grads), list(m), list(v)
     n = len(params)
     scales = None if scales is None else list(scales)
