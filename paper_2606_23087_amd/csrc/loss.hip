@@ -861,23 +861,24 @@ __device__ __forceinline__ void finish_row(const LossArgs& a, int32_t t, int32_t
 }
 
 // Adds up the rows at places `from` to `to` of the order, each times its gradient
-// at the label, 8 columns a lane from c on: every fourth row, 8 under way.
-template <class T>
+// at the label, 8 columns a lane from c on: every kWaves-th row from the wave's
+// on, 8 under way.
+template <class T, int kWaves>
 __device__ __forceinline__ void add_rows(const LossArgs& a, const Classes& o, int32_t from, int32_t to, int32_t c, float (&s)[8]) {
-  for (int32_t k = from + uniform(threadIdx.x >> 6); k < to; k += 32) {
+  for (int32_t k = from + uniform(threadIdx.x >> 6) % kWaves; k < to; k += 8 * kWaves) {
     int32_t row[8];
     float own[8];
     Pack<T, 8> x[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) row[e] = o.order[min(k + 4 * e, to - 1)];
+    for (int e = 0; e < 8; ++e) row[e] = o.order[min(k + kWaves * e, to - 1)];
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      own[e] = k + 4 * e < to ? a.own[row[e]] : 0.f;
+      own[e] = a.own[row[e]];
       x[e] = load<T, 8>((const T*)a.xc + (int64_t)row[e] * a.ld + c);
     }
 #pragma unroll
     for (int e = 0; e < 8; ++e)
-      if (k + 4 * e < to)
+      if (k + kWaves * e < to)
 #pragma unroll
         for (int d = 0; d < 8; ++d) s[d] += own[e] * x[e].get(d);
   }
@@ -908,7 +909,7 @@ __global__ __launch_bounds__(256) void k_class_parts(LossArgs a, Classes o) {
   if (i + kPart > *a.count || a.picks[o.order[i]] != a.picks[o.order[i + kPart - 1]]) return;
   const int32_t c = blockIdx.y * 512 + (threadIdx.x & 63) * 8;
   float s[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-  add_rows<T>(a, o, i, i + kPart, min(c, a.hidden - 8), s);
+  add_rows<T, 4>(a, o, i, i + kPart, min(c, a.hidden - 8), s);
   join_waves(s, parts);
   if (threadIdx.x < 64 && c < a.hidden) {
     Pack<float, 8> p;
@@ -918,9 +919,24 @@ __global__ __launch_bounds__(256) void k_class_parts(LossArgs a, Classes o) {
   }
 }
 
+// 8 elements of a class's row of dweight: the pieces' sums p and its own rows' s.
+template <class O>
+__device__ __forceinline__ void finish_vector(O* to, const Pack<float, 8>& p, const float (&s)[8], float f, int32_t add) {
+  Pack<O, 8> out;
+  Pack<float, 8> old{};
+  if constexpr (__is_same(O, float))
+    if (add) old = load<float, 8>(to);
+#pragma unroll
+  for (int d = 0; d < 8; ++d) out.set(d, old.get(d) + f * (p.get(d) + s[d]));
+  store<O, 8>(to, out);
+}
+
 // The row of dweight of the class whose rows begin at place i: its sums over the
 // piece's product, and each of its own rows times that row's gradient at the
-// label. 512 columns at a time.
+// label, 512 columns at a time. The rows of a class that has few are added up by
+// each of the 4 waves for its own columns, those of others by all 4 waves for the
+// same columns (16384 rows over 8192 x 2048, two a class: 168 us if all were).
+constexpr int32_t kFewRows = 16;
 template <class T, class O>
 __device__ __forceinline__ void finish_class(const LossArgs& a, const Classes& o, int32_t i, float f, O* dweight, int64_t dw_ld,
                                              int32_t add, bool in_parts) {
@@ -928,34 +944,33 @@ __device__ __forceinline__ void finish_class(const LossArgs& a, const Classes& o
   const int32_t many = uniform(o.many[i]);
   if (!many) return;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int64_t v = a.picks[o.order[i]];
+  O* const row = dweight + (int64_t)a.picks[o.order[i]] * dw_ld;
+  const float* const side = a.side + (int64_t)i * a.ld;
+  const int32_t from = blockIdx.y * 2048, to = min(a.hidden, from + 2048);
+  if (many <= kFewRows) {
+    const int32_t c = from + wave * 512 + lane * 8;
+    if (c >= to) return;
+    const Pack<float, 8> p = load<float, 8>(side + c);
+    float s[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+    add_rows<T, 1>(a, o, i, i + many, c, s);
+    return finish_vector(row + c, p, s, f, add);
+  }
   // places up to the first whole part, whole parts, and places behind the last; without whole parts all are the first
   int32_t whole = (i + kPart - 1) / kPart, end = (i + many) / kPart;
   if (!in_parts || whole >= end) whole = end = (i + many + kPart - 1) / kPart;
-  for (int32_t c0 = blockIdx.y * 2048; c0 < min(a.hidden, (int32_t)(blockIdx.y + 1) * 2048); c0 += 512) {
+  for (int32_t c0 = from; c0 < to; c0 += 512) {
     const int32_t c = c0 + lane * 8, at = min(c, a.hidden - 8);
     float s[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-    add_rows<T>(a, o, i, min(whole * kPart, i + many), at, s);
+    add_rows<T, 4>(a, o, i, min(whole * kPart, i + many), at, s);
 #pragma unroll 8
     for (int32_t k = whole + wave; k < end; k += 4) {
       const Pack<float, 8> p = load<float, 8>(a.side + (int64_t)(k * kPart + 1) * a.ld + at);
 #pragma unroll
       for (int d = 0; d < 8; ++d) s[d] += p.get(d);
     }
-    add_rows<T>(a, o, min(end * kPart, i + many), i + many, at, s);
+    add_rows<T, 4>(a, o, min(end * kPart, i + many), i + many, at, s);
     join_waves(s, parts);
-    if (!wave && c < a.hidden) {
-      const Pack<float, 8> p = load<float, 8>(a.side + (int64_t)i * a.ld + c);
-      O* const to = dweight + v * dw_ld + c;
-      Pack<O, 8> out;
-      Pack<float, 8> old{};
-      if constexpr (__is_same(O, float))
-        if (add) old = load<float, 8>(to);
-#pragma unroll
-      for (int d = 0; d < 8; ++d)
-        out.set(d, old.get(d) + f * (p.get(d) + s[d]));
-      store<O, 8>(to, out);
-    }
+    if (!wave && c < to) finish_vector(row + c, load<float, 8>(side + c), s, f, add);
   }
 }
 
